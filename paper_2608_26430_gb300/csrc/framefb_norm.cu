@@ -8,6 +8,7 @@
 
 #include "framefb.h"
 #include "framefb_norm.cuh"
+#include "framefb_smem.h"
 
 namespace {
 
@@ -182,9 +183,10 @@ bool dtype_ok(framefb_dtype dt) { return dt == FRAMEFB_F32 || dt == FRAMEFB_BF16
 // dependent launch; it waits by itself).
 framefb_status launch(KernelFn f, dim3 blocks, int threads, size_t smem, void* args, bool chained, void* stream) {
   void* kargs[] = {args};
-  if (smem > 24 * 1024 &&  // with the kernels' static 24 KB over what needs no opt-in
-      cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
-    return FRAMEFB_ECUDA;
+  if (smem > 24 * 1024) {  // with the kernels' static 24 KB over what needs no opt-in
+    const framefb_status st = ffb_host::allow_smem(f);
+    if (st != FRAMEFB_OK) return st;
+  }
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;

@@ -1,0 +1,73 @@
+"""Calls from several host threads, each with a stream of its own: a call's
+launch does not depend on what another thread launches with the same kernel."""
+import threading
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2608_26430_gb300 import framefb as ffb
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2608_26430_gb300.build import build
+    build()
+    ffb.lib()
+
+
+def at_once(calls, times):
+    """Each of `calls` (a function of a stream) `times` times in a thread of its own; the errors they raised."""
+    errors, gate = [], threading.Barrier(len(calls))
+
+    def work(call):
+        stream = torch.cuda.Stream()
+        gate.wait()
+        try:
+            for i in range(times):
+                call(stream)
+                if i % 200 == 199:
+                    stream.synchronize()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    return errors
+
+
+def test_norms_of_unlike_shared_memory():
+    # one kernel of the gradient, with a third input (96 KB of shared memory) and without (64 KB); the descriptors
+    # are laid out before, so that the threads meet in the library and not at the interpreter's lock
+    N, d = 2, 4096
+    g = torch.Generator(device=DEV).manual_seed(1)
+    dY, Z, dZin = (torch.randn((N, d), generator=g, device=DEV).bfloat16() for _ in range(3))
+    mean, rstd = torch.zeros(N, device=DEV), torch.ones(N, device=DEV)
+    outs, want = ([torch.empty_like(dY) for _ in range(4)] for _ in range(2))
+    for i, o in enumerate(want):
+        ffb.framefb_layernorm_backward(dY, Z, None, mean, rstd, o, dZin=(None, dZin)[i % 2])
+
+    def call(i):
+        rows = lambda t: (t.data_ptr(), d)  # noqa: E731
+        s = ffb._NORM.pack(N, d, 0.0, 0, 0, 0, mean.data_ptr(), rstd.data_ptr(), *rows(Z), 0, 0, 0, 0, 0, 0, *rows(dY),
+                           *(rows(dZin) if i % 2 else (0, 0)), *rows(outs[i]), 0, 0, 0, 0)
+        f = ffb.lib().framefb_layernorm_backward
+
+        def run(stream):
+            status = f(s, ffb.FRAMEFB_BF16, None, 0, stream.cuda_stream)
+            if status != ffb.FRAMEFB_OK:
+                raise ffb.FramefbError(status, "framefb_layernorm_backward")
+        return run
+    assert at_once([call(i) for i in range(4)], 4000) == []
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
