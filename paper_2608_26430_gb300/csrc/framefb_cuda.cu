@@ -13,6 +13,7 @@
 
 #include "framefb.h"
 #include "framefb_dense.h"
+#include "framefb_smem.h"
 #include "framefb_xent.h"
 #include "framefb_kernels.cuh"
 #include "framefb_mma.cuh"
@@ -544,9 +545,8 @@ framefb_status prepare(const framefb_mat* mats, int32_t nmats, int32_t ops, fram
   int dev = 0, sms = 0, per_sm = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return FRAMEFB_ECUDA;
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return FRAMEFB_ECUDA;
-  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(P.smem)) !=
-      cudaSuccess)
-    return FRAMEFB_ECUDA;
+  const framefb_status allowed = ffb_host::allow_smem(fn);
+  if (allowed != FRAMEFB_OK) return allowed;
   if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, P.threads, P.smem) != cudaSuccess)
     return FRAMEFB_ECUDA;
   if (per_sm < 1) return FRAMEFB_EUNSUPPORTED;

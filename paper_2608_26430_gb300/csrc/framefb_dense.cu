@@ -25,6 +25,7 @@
 #include "framefb.h"
 #include "framefb_dense.cuh"
 #include "framefb_dense.h"
+#include "framefb_smem.h"
 #include "plan_internal.h"
 #include "plan_layout.h"
 
@@ -286,8 +287,8 @@ GemmKind sy_kernel(bool grouped) {
 // Queue one contraction launch over `L` (problems filled, tiles counted).
 framefb_status launch_gemm(const GemmKind& k, fd::GemmLaunch& L, int sms, cudaStream_t st) {
   if (L.total_tiles == 0) return FRAMEFB_OK;
-  if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem)) != cudaSuccess)
-    return FRAMEFB_ECUDA;
+  const framefb_status allowed = allow_smem(k.fn);
+  if (allowed != FRAMEFB_OK) return allowed;
   const int grid = std::min(L.total_tiles, sms * k.per_sm);
   void* args[] = {&L};
   if (cudaLaunchKernel(k.fn, dim3(grid), dim3(fd::kGemmThreads), args, k.smem, st) != cudaSuccess)
@@ -453,10 +454,9 @@ framefb_status dense_run(const framefb_mat* mats, int32_t nmats, int32_t ops, fr
         const int64_t units = (Nc + p.TT - 1) / p.TT;
         const int grid = static_cast<int>(std::min<int64_t>(units, g.grid));
         void* fn = spmm_kernel_ptr(p.mode, p.TT, spmm_e(h));
-        if (!fn ||
-            cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(p.smem)) !=
-                cudaSuccess)
-          return FRAMEFB_ECUDA;
+        if (!fn) return FRAMEFB_ECUDA;
+        const framefb_status allowed = allow_smem(fn);
+        if (allowed != FRAMEFB_OK) return allowed;
         void* args[] = {&a};
         if (cudaLaunchKernel(fn, dim3(grid), dim3(fd::kSpmmThreads), args, p.smem, st) != cudaSuccess)
           return FRAMEFB_ECUDA;

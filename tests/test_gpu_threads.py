@@ -7,6 +7,8 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2608_26430_gb300 import framefb as ffb
+from paper_2608_26430_gb300 import workloads as wl
+from paper_2608_26430_gb300.batch import AdapterBatch
 
 pytestmark = pytest.mark.gpu
 
@@ -27,6 +29,7 @@ def at_once(calls, times):
     errors, gate = [], threading.Barrier(len(calls))
 
     def work(call):
+        torch.cuda.set_device(DEV)
         stream = torch.cuda.Stream()
         gate.wait()
         try:
@@ -71,3 +74,23 @@ def test_norms_of_unlike_shared_memory():
         return run
     assert at_once([call(i) for i in range(4)], 4000) == []
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("dtype,dims,rho2", [("f32", (256, 768), False), ("bf16", (256, 768), False), ("bf16", (384, 768), True)])
+def test_adapters_of_unlike_shared_memory(dtype, dims, rho2):
+    # two widths of one kernel, of the structured and of the contraction path
+    def batch(d, ops=7):
+        frames = ((d, d // 2, 2),) if rho2 else ()
+        w = wl.Workload(f"threads_{d}", (wl.MatSpec("w", d, d),), N=64, nnz=128, dtype=dtype, c_std=0.02, frames=frames)
+        b = AdapterBatch(w, DEV, ops=ops)
+        return b, b.workspace(ops)
+    batches, alone = [batch(d) for d in dims], [batch(d) for d in dims]
+    times = 600
+
+    def call(b, ws):
+        return lambda stream: ffb.framefb_run(b.mats, ffb.OP_BACKWARD_DX | ffb.OP_GRAD_COEFF, b.dtype_code, ws, stream)
+    for b, ws in alone:
+        call(b, ws)(None)
+    assert at_once([call(b, ws) for b, ws in batches], times) == []
+    for (a, _), (b, _) in zip(batches, alone):
+        assert torch.equal(a.dC, b.dC)
