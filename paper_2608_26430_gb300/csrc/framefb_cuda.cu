@@ -545,7 +545,7 @@ framefb_status prepare(const framefb_mat* mats, int32_t nmats, int32_t ops, fram
   int dev = 0, sms = 0, per_sm = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return FRAMEFB_ECUDA;
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return FRAMEFB_ECUDA;
-  const framefb_status allowed = ffb_host::allow_smem(fn);
+  const framefb_status allowed = ffb_host::allow_smem(fn, P.smem);
   if (allowed != FRAMEFB_OK) return allowed;
   if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, P.threads, P.smem) != cudaSuccess)
     return FRAMEFB_ECUDA;

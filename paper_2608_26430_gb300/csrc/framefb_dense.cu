@@ -287,7 +287,7 @@ GemmKind sy_kernel(bool grouped) {
 // Queue one contraction launch over `L` (problems filled, tiles counted).
 framefb_status launch_gemm(const GemmKind& k, fd::GemmLaunch& L, int sms, cudaStream_t st) {
   if (L.total_tiles == 0) return FRAMEFB_OK;
-  const framefb_status allowed = allow_smem(k.fn);
+  const framefb_status allowed = allow_smem(k.fn, k.smem);
   if (allowed != FRAMEFB_OK) return allowed;
   const int grid = std::min(L.total_tiles, sms * k.per_sm);
   void* args[] = {&L};
@@ -455,7 +455,7 @@ framefb_status dense_run(const framefb_mat* mats, int32_t nmats, int32_t ops, fr
         const int grid = static_cast<int>(std::min<int64_t>(units, g.grid));
         void* fn = spmm_kernel_ptr(p.mode, p.TT, spmm_e(h));
         if (!fn) return FRAMEFB_ECUDA;
-        const framefb_status allowed = allow_smem(fn);
+        const framefb_status allowed = allow_smem(fn, p.smem);
         if (allowed != FRAMEFB_OK) return allowed;
         void* args[] = {&a};
         if (cudaLaunchKernel(fn, dim3(grid), dim3(fd::kSpmmThreads), args, p.smem, st) != cudaSuccess)

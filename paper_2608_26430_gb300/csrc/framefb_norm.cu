@@ -184,7 +184,7 @@ bool dtype_ok(framefb_dtype dt) { return dt == FRAMEFB_F32 || dt == FRAMEFB_BF16
 framefb_status launch(KernelFn f, dim3 blocks, int threads, size_t smem, void* args, bool chained, void* stream) {
   void* kargs[] = {args};
   if (smem > 24 * 1024) {  // with the kernels' static 24 KB over what needs no opt-in
-    const framefb_status st = ffb_host::allow_smem(f);
+    const framefb_status st = ffb_host::allow_smem(f, smem);
     if (st != FRAMEFB_OK) return st;
   }
   cudaLaunchAttribute attr{};
