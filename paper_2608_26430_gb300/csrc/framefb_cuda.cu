@@ -296,23 +296,18 @@ size_t tc2_smem_map(const framefb_mat* mats, int32_t nmats, int32_t ops, int S, 
   return mbar + 8 * static_cast<size_t>(S + 3);  // stages, analysis, synthesis, RZ/RG written
 }
 
-using ffb_host::encode_tiled;
-using ffb_host::EncodeTiledFn;
+using ffb_host::can_encode;
+using ffb_host::encode_map;
 
 // Tensor map of the bf16 rows of one activation tensor (d features, N
 // tokens, leading dimension ld elements): {32 coordinates, d / 32 groups, N
 // tokens}, box {32, d / 32, rows} (rows consecutive tokens, one row per
 // group, token-major), 64-byte swizzle.
 bool encode_rows(CUtensorMap* map, const void* base, int32_t d, int32_t N, int64_t ld, int32_t rows = 1) {
-  const EncodeTiledFn fn = encode_tiled();
-  if (!fn) return false;
   const cuuint64_t dims[3] = {32, static_cast<cuuint64_t>(d / 32), static_cast<cuuint64_t>(N)};
   const cuuint64_t strides[2] = {64, static_cast<cuuint64_t>(ld) * 2};
   const cuuint32_t box[3] = {32, static_cast<cuuint32_t>(d / 32), static_cast<cuuint32_t>(rows)};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 // Kernel choice for bf16: the two-token tensor-core kernel wherever it
@@ -360,7 +355,7 @@ framefb_status prepare(const framefb_mat* mats, int32_t nmats, int32_t ops, fram
   bool tc = false, tc2 = false;
   int pairs[ffb::kTcMaxMats];
   bool pack = false;
-  if (dt == FRAMEFB_BF16 && reg && tc2_allowed() && nmats <= ffb::kTcMaxMats && encode_tiled()) {
+  if (dt == FRAMEFB_BF16 && reg && tc2_allowed() && nmats <= ffb::kTcMaxMats && can_encode()) {
     // two-token tensor-core kernel: two stages; small dimensions pack
     // several token pairs per unit
     for (int32_t j = 0; j < nmats; ++j) {
@@ -390,7 +385,7 @@ framefb_status prepare(const framefb_mat* mats, int32_t nmats, int32_t ops, fram
       smem = tc2_smem_map(mats, nmats, ops, 2, pairs, pack, P.tcargs);
     }
   }
-  if (dt == FRAMEFB_BF16 && reg && !tc2 && tc_allowed() && nmats <= ffb::kTcMaxMats && encode_tiled()) {
+  if (dt == FRAMEFB_BF16 && reg && !tc2 && tc_allowed() && nmats <= ffb::kTcMaxMats && can_encode()) {
     // tensor-core pipelined kernel: deepest staging ring (2..4) that fits
     int dev = 0, optin = 0;
     cudaFuncAttributes fa{};

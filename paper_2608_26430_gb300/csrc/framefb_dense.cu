@@ -31,6 +31,10 @@
 
 namespace ffb_host {
 
+namespace {
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiledFn encode_tiled() {
   static const EncodeTiledFn fn = [] {
     void* p = nullptr;
@@ -42,6 +46,25 @@ EncodeTiledFn encode_tiled() {
     return reinterpret_cast<EncodeTiledFn>(p);
   }();
   return fn;
+}
+}  // namespace
+
+bool can_encode() { return encode_tiled() != nullptr; }
+
+bool encode_map(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims,
+                const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
+  const EncodeTiledFn fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  auto encode = [&] {
+    return fn(map, type, static_cast<cuuint32_t>(rank), const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (encode()) return true;
+  // the thread may have no current context yet: cudaSetDevice gives it one
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode();
 }
 
 namespace {
@@ -227,15 +250,11 @@ std::vector<const framefb_dev_frame*> block_frames(const framefb_mat* mats, int3
 // {128 bytes of columns, box_rows rows}, 128-byte swizzle, zeros outside.
 bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, int esz, const void* base, int64_t cols, int64_t rows,
                int64_t pitch, int box_rows) {
-  const EncodeTiledFn fn = encode_tiled();
-  if (!fn || cols <= 0 || rows <= 0) return false;
+  if (cols <= 0 || rows <= 0) return false;
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch)};
   const cuuint32_t box[2] = {static_cast<cuuint32_t>(fd::kRowBytes / esz), static_cast<cuuint32_t>(box_rows)};
-  const cuuint32_t estr[2] = {1, 1};
-  return fn(map, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
-         CUDA_SUCCESS;
+  return encode_map(map, type, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 void* spmm_kernel_ptr(int mode, int TT, int E) {
@@ -347,7 +366,7 @@ framefb_status dense_check(const framefb_mat* mats, int32_t nmats, int32_t ops, 
   *ws_need = 0;
   if (nmats == 0) return FRAMEFB_OK;
   if (dt != FRAMEFB_BF16) return FRAMEFB_EUNSUPPORTED;  // this path takes bf16 activations
-  if (!encode_tiled()) return FRAMEFB_ECUDA;
+  if (!can_encode()) return FRAMEFB_ECUDA;
   const int sms = sm_count();
   if (sms <= 0) return FRAMEFB_ECUDA;
   size_t region = 0;

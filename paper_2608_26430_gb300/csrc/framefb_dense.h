@@ -12,11 +12,14 @@
 namespace ffb_host {
 
 // cuTensorMapEncodeTiled through the runtime's driver entry point (no link
-// against the driver library); NULL when the driver does not provide it.
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled();
+// against the driver library).  `rank` dimensions, `rank` - 1 strides (bytes),
+// boxes without gaps, zeros outside; false when the driver refuses the map.
+// Works on a host thread without earlier CUDA work: the driver's call needs a
+// current context, and such a thread gets the current device's.
+bool encode_map(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims,
+                const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swizzle);
+// The driver has it.
+bool can_encode();
 
 // Validate the dense-path matrices of a call (plans with FFB_LAYOUT_DENSE)
 // and report the workspace they need (bytes; the matrices run one after

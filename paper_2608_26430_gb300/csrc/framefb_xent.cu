@@ -104,15 +104,10 @@ Plan plan_of(int64_t N, int32_t d, int32_t V, int32_t ops, int pairs) {
 
 // Tensor map of a row-major bf16 [rows][cols] array in 64 x 64 boxes.
 bool encode(CUtensorMap* map, const void* base, int64_t cols, int64_t rows, int64_t ld) {
-  const ffb_host::EncodeTiledFn fn = ffb_host::encode_tiled();
-  if (!fn) return false;
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
   const cuuint32_t box[2] = {64, 64};
-  const cuuint32_t estr[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return ffb_host::encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 bool rows_ok(const void* p, int64_t ld, int32_t d) {

@@ -9,6 +9,7 @@ torch = pytest.importorskip("torch")
 from paper_2608_26430_gb300 import framefb as ffb
 from paper_2608_26430_gb300 import workloads as wl
 from paper_2608_26430_gb300.batch import AdapterBatch
+from tests.test_gpu_xent import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +95,58 @@ def test_adapters_of_unlike_shared_memory(dtype, dims, rho2):
     assert at_once([call(b, ws) for b, ws in batches], times) == []
     for (a, _), (b, _) in zip(batches, alone):
         assert torch.equal(a.dC, b.dC)
+
+
+def in_new_thread(call):
+    """What `call` raised as the first CUDA work of a host thread (None: nothing)."""
+    got = []
+
+    def work():
+        try:
+            call()
+            got.append(None)
+        except Exception as e:  # noqa: BLE001
+            got.append(e)
+    torch.cuda.synchronize()
+    t = threading.Thread(target=work)
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    return got[0]
+
+
+@pytest.mark.parametrize("rho2", [False, True])
+def test_adapters_as_a_threads_first_work(rho2):
+    w = wl.Workload("thread", (wl.MatSpec("w", 384, 384),), N=64, nnz=128, dtype="bf16", c_std=0.02,
+                    frames=((384, 192, 2),) if rho2 else ())
+    b = AdapterBatch(w, DEV)
+    ws = b.workspace(7)
+    b.run(7, ws)
+    want = b.dC.clone()
+    b.dC.zero_()
+    assert in_new_thread(lambda: b.run(7, ws, stream=0)) is None
+    assert torch.equal(b.dC, want)
+
+
+@pytest.mark.parametrize("N", [1, 64])
+def test_cross_entropy_as_a_threads_first_work(N):
+    c = Case(N, 72, 300)
+    want = c.forward()
+    grads = c.backward(want[1])
+    got = [torch.empty_like(x) for x in want]
+    ws = [ffb.xent_workspace(N, 72, 300, ops, DEV) for ops in (ffb.XENT_FORWARD, ffb.XENT_DH | ffb.XENT_DW)]
+    dH, dW = c.H.clone(), c.W.clone()
+    assert in_new_thread(lambda: ffb.framefb_xent_forward(c.H, c.W, c.t, *got, ws=ws[0], stream=0)) is None
+    assert in_new_thread(lambda: ffb.framefb_xent_backward(c.H, c.W, c.t, want[1], dH=dH, dW=dW, ws=ws[1], stream=0)) is None
+    for a, b in zip(got + [dH, dW], want + grads):
+        assert torch.equal(a, b)
+
+
+def test_norm_and_dropout_as_a_threads_first_work():
+    x = torch.randn((8, 768), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).bfloat16()
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    for call in (lambda o: ffb.framefb_layernorm_forward(x, None, None, o, stream=0),
+                 lambda o: ffb.framefb_dropout(x, o, 0.5, 3, stream=0)):
+        call(y)
+        assert in_new_thread(lambda: call(z)) is None
+        assert torch.equal(y, z)
