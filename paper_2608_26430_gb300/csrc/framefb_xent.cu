@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <initializer_list>
 
 #include "framefb.h"
 #include "framefb_dense.h"
@@ -211,9 +212,17 @@ framefb_status launch_grads(int64_t mt, bool join, int pairs, const fx::GemmArgs
 framefb_status check(const framefb_xent* x, framefb_dtype dtype) {
   if (!x || (dtype != FRAMEFB_BF16 && dtype != FRAMEFB_F32) || !sizes_ok(x->N, x->d, x->V)) return FRAMEFB_EINVAL;
   if (dtype != FRAMEFB_BF16) return FRAMEFB_EUNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(x->target) % 8) return FRAMEFB_EINVAL;
   if (x->N > 0 && (!rows_ok(x->H, x->ldh, x->d) || !rows_ok(x->W, x->ldw, x->d) || !x->target || !x->lse))
     return FRAMEFB_EINVAL;
   return FRAMEFB_OK;
+}
+
+// fp32 vectors (NULL passes), in the direction that looks at them.
+bool aligned4(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (reinterpret_cast<uintptr_t>(p) % 4) return false;
+  return true;
 }
 
 framefb_status check_ws(const Plan& p, const void* ws, size_t ws_bytes) {
@@ -272,6 +281,7 @@ extern "C" size_t framefb_xent_workspace_size(int64_t N, int32_t d, int32_t V, i
 extern "C" framefb_status framefb_xent_forward(const framefb_xent* x, framefb_dtype dtype, void* ws, size_t ws_bytes,
                                                void* stream) {
   FFB_TRY(check(x, dtype));
+  if (!aligned4({x->loss, x->lse, x->loss_mean})) return FRAMEFB_EINVAL;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (x->N == 0) {
     if (x->loss_mean && cudaMemsetAsync(x->loss_mean, 0, sizeof(float), st) != cudaSuccess) return FRAMEFB_ECUDA;
@@ -342,6 +352,7 @@ extern "C" framefb_status framefb_xent_forward(const framefb_xent* x, framefb_dt
 extern "C" framefb_status framefb_xent_backward(const framefb_xent* x, framefb_dtype dtype, void* ws, size_t ws_bytes,
                                                 void* stream) {
   FFB_TRY(check(x, dtype));
+  if (!aligned4({x->lse, x->dloss})) return FRAMEFB_EINVAL;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (!std::isfinite(x->scale) || (x->dH && !rows_ok(x->dH, x->lddh, x->d)) || (x->dW && !rows_ok(x->dW, x->lddw, x->d)))
     return FRAMEFB_EINVAL;
