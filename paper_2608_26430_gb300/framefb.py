@@ -45,6 +45,14 @@ class FramefbError(RuntimeError):
         super().__init__(f"{what}: {status_string(status)} ({status})")
 
 
+class FramefbDeviceError(FramefbError, ValueError):
+    """Tensors that are not on the current CUDA device."""
+
+    def __init__(self, what: str, dev: int):
+        super().__init__(FRAMEFB_EINVAL, f"{what} of tensors on {'the CPU' if dev < 0 else f'cuda:{dev}'}, "
+                                         f"which is not the current CUDA device")
+
+
 class framefb_frame_params(ct.Structure):
     _fields_ = [("k", ct.c_int32), ("rho", ct.c_int32), ("parseval", ct.c_int32)]
 
@@ -494,12 +502,32 @@ def _vec(t, name: str, n: int, dtype, dev: int) -> int:
     return t.data_ptr()
 
 
-def _ws(ws):
-    return (0, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+def _ws(ws, dev: int):
+    if ws is None:
+        return 0, 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous and on the activations' device")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _drop(drop) -> int:
     return 0 if drop is None else ct.addressof(drop)
+
+
+def _queue(stream, dev: int):
+    """Raw stream for work on tensors of device `dev`; None where that is not
+    the current CUDA device, whose streams and memory the library uses."""
+    import torch
+    if dev < 0 or torch.cuda.current_device() != dev:
+        return None
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+
+
+def _refuse_device(name: str, dev: int, status: int):
+    """`status`: of the same call without rows, which looks at sizes and types
+    only; what is wrong with those comes first."""
+    _check(status, name)
+    raise FramefbDeviceError(name, dev)
 
 
 def framefb_dropout(X, Y, p: float, seed: int, offset: int = 0, R=None, stream=None) -> None:
@@ -509,8 +537,16 @@ def framefb_dropout(X, Y, p: float, seed: int, offset: int = 0, R=None, stream=N
     a = _Like(X)
     N, d = a.shape
     k = framefb_dropout_params(p, seed, offset)
-    _check(lib().framefb_dropout(*_rows(X, "X", a), *_rows(R, "R", a), *_rows(Y, "Y", a), N, d, _dtype_code(X),
-                                 ct.byref(k), _stream(stream)), "framefb_dropout")
+    x, r, y, code = _rows(X, "X", a), _rows(R, "R", a), _rows(Y, "Y", a), _dtype_code(X)
+    q = _queue(stream, a.dev) if N > 0 else 0
+    if q is None:
+        _refuse_device("framefb_dropout", a.dev, lib().framefb_dropout(0, d, 0, d, 0, d, 0, d, code, ct.byref(k), 0))
+    _check(lib().framefb_dropout(*x, *r, *y, N, d, code, ct.byref(k), q), "framefb_dropout")
+
+
+def _refuse_norm(name: str, a: _Like, eps: float, drop, code: int):
+    s = _NORM.pack(0, a.shape[1], eps, _drop(drop), *[0] * 22)
+    _refuse_device(name, a.dev, lib().framefb_layernorm_forward(s, code, 0))
 
 
 def framefb_layernorm_forward(X, gamma, beta, Y, mean=None, rstd=None, eps: float = 1e-5, R=None, Z=None, drop=None,
@@ -525,7 +561,11 @@ def framefb_layernorm_forward(X, gamma, beta, Y, mean=None, rstd=None, eps: floa
     s = _NORM.pack(N, d, eps, _drop(drop), _vec(gamma, "gamma", d, f32, dev), _vec(beta, "beta", d, f32, dev),
                    _vec(mean, "mean", N, f32, dev), _vec(rstd, "rstd", N, f32, dev), *_rows(Z, "Z", a),
                    *_rows(X, "X", a), *_rows(R, "R", a), *_rows(Y, "Y", a), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
-    _check(lib().framefb_layernorm_forward(s, _dtype_code(X), _stream(stream)), "framefb_layernorm_forward")
+    code = _dtype_code(X)
+    q = _queue(stream, dev) if N > 0 else 0
+    if q is None:
+        _refuse_norm("framefb_layernorm_forward", a, eps, drop, code)
+    _check(lib().framefb_layernorm_forward(s, code, q), "framefb_layernorm_forward")
 
 
 def framefb_layernorm_workspace_size(N: int, d: int) -> int:
@@ -535,7 +575,8 @@ def framefb_layernorm_workspace_size(N: int, d: int) -> int:
 def layernorm_workspace(N: int, d: int, device):
     """Caller-side workspace tensor for dgamma and dbeta of framefb_layernorm_backward."""
     import torch
-    n = framefb_layernorm_workspace_size(N, d)
+    with torch.cuda.device(device):  # the size depends on the device
+        n = framefb_layernorm_workspace_size(N, d)
     return torch.empty(n, dtype=torch.uint8, device=device) if n > 0 else None
 
 
@@ -551,8 +592,12 @@ def framefb_layernorm_backward(dY, Z, gamma, mean, rstd, dZ=None, dgamma=None, d
                    _vec(rstd, "rstd", N, f32, dev), *_rows(Z, "Z", a), 0, 0, 0, 0, 0, 0, *_rows(dY, "dY", a),
                    *_rows(dZin, "dZin", a), *_rows(dZ, "dZ", a), *_rows(dX, "dX", a),
                    _vec(dgamma, "dgamma", d, f32, dev), _vec(dbeta, "dbeta", d, f32, dev))
-    wp, wb = _ws(ws)
-    _check(lib().framefb_layernorm_backward(s, _dtype_code(dY), wp, wb, _stream(stream)), "framefb_layernorm_backward")
+    wp, wb = _ws(ws, dev)
+    code = _dtype_code(dY)
+    q = _queue(stream, dev) if N > 0 or dgamma is not None or dbeta is not None else 0
+    if q is None:
+        _refuse_norm("framefb_layernorm_backward", a, 0.0, drop, code)
+    _check(lib().framefb_layernorm_backward(s, code, wp, wb, q), "framefb_layernorm_backward")
 
 
 def framefb_xent_workspace_size(N: int, d: int, V: int, ops: int) -> int:
@@ -563,7 +608,8 @@ def xent_workspace(N: int, d: int, V: int, ops: int, device):
     """Caller-side workspace tensor for framefb_xent_forward (ops XENT_FORWARD)
     or framefb_xent_backward (XENT_DH and / or XENT_DW)."""
     import torch
-    n = framefb_xent_workspace_size(N, d, V, ops)
+    with torch.cuda.device(device):  # the size depends on the device
+        n = framefb_xent_workspace_size(N, d, V, ops)
     return torch.empty(n, dtype=torch.uint8, device=device) if n > 0 else None
 
 
@@ -582,13 +628,22 @@ def _xent(H, W, target, lse, loss=None, loss_mean=None, ignore_index=-100, dloss
                       *_rows(dW, "dW", w), scale, 0)
 
 
+def _refuse_xent(name: str, H, W):
+    s = _XENT.pack(0, H.shape[1], W.shape[0], *[0] * 14, 0.0, 0)
+    _refuse_device(name, H.get_device(), lib().framefb_xent_forward(s, _dtype_code(H), 0, 0, 0))
+
+
 def framefb_xent_forward(H, W, target, loss, lse, loss_mean=None, ignore_index: int = -100, ws=None,
                          stream=None) -> None:
     """Cross entropy of the logits H W^T per token (loss, lse) and its mean
     over the tokens whose target is not ignore_index; no logits are stored."""
     s = _xent(H, W, target, lse, loss, loss_mean, ignore_index)
-    wp, wb = _ws(ws)
-    _check(lib().framefb_xent_forward(s, _dtype_code(H), wp, wb, _stream(stream)), "framefb_xent_forward")
+    dev = H.get_device()
+    wp, wb = _ws(ws, dev)
+    q = _queue(stream, dev) if H.shape[0] > 0 or loss_mean is not None else 0
+    if q is None:
+        _refuse_xent("framefb_xent_forward", H, W)
+    _check(lib().framefb_xent_forward(s, _dtype_code(H), wp, wb, q), "framefb_xent_forward")
 
 
 def framefb_xent_backward(H, W, target, lse, dH=None, dW=None, dloss=None, scale: float = 1.0,
@@ -596,8 +651,12 @@ def framefb_xent_backward(H, W, target, lse, dH=None, dW=None, dloss=None, scale
     """Gradients of scale * sum_t dloss_t loss_t (dloss None: of scale * the
     mean loss) with the forward pass's lse; dH and dW each where given."""
     s = _xent(H, W, target, lse, ignore_index=ignore_index, dloss=dloss, dH=dH, dW=dW, scale=scale)
-    wp, wb = _ws(ws)
-    _check(lib().framefb_xent_backward(s, _dtype_code(H), wp, wb, _stream(stream)), "framefb_xent_backward")
+    dev = H.get_device()
+    wp, wb = _ws(ws, dev)
+    q = _queue(stream, dev) if dW is not None or (dH is not None and H.shape[0] > 0) else 0
+    if q is None:
+        _refuse_xent("framefb_xent_backward", H, W)
+    _check(lib().framefb_xent_backward(s, _dtype_code(H), wp, wb, q), "framefb_xent_backward")
 
 
 def framefb_wait_timeouts() -> int:
