@@ -490,7 +490,7 @@ def _rows(t, name: str, like: _Like):
     ld, cs = t.stride()
     if cs != 1 and d > 1:
         raise ValueError(f"{name} must have unit column stride")
-    return t.data_ptr(), ld if n > 1 or ld > d else d  # one row has no stride that matters
+    return t.data_ptr(), ld if n > 1 else -(-d // 8) * 8  # one row has no stride that matters
 
 
 def _vec(t, name: str, n: int, dtype, dev: int) -> int:

@@ -98,3 +98,12 @@ def test_workspaces():
                      lambda: ffb.framefb_xent_backward(h, w, t, v, dH=h, ws=ws, stream=0)):
             with pytest.raises(ValueError, match="ws"):
                 call()
+
+
+@pytest.mark.parametrize("d", [1, 12, 16])
+def test_the_stride_of_one_row_does_not_matter(d):
+    # one token out of a wider buffer, or broadcast: its row starts where it starts
+    for t in (torch.zeros(2, 17)[:1, :d], torch.zeros(3, d)[1:2], torch.zeros(d).expand(1, d)):
+        ptr, ld = ffb._rows(t, "t", ffb._Like(t))
+        assert ptr == t.data_ptr() and ld >= d and ld % 8 == 0
+    assert ffb._rows(torch.zeros(2, 17)[:, :d], "t", ffb._Like(torch.zeros(2, d)))[1] == 17
