@@ -157,6 +157,14 @@ int32_t piece_bytes(int32_t d, int esz) { return static_cast<int32_t>((static_ca
 
 // Rows of the ring: what fits beside `params` bytes, up to 4 (1: the row at work only).
 constexpr size_t kSmemPerSm = 210 * 1024;
+// The same of each of two forward blocks on an SM: 105 KB, or 101 beside the
+// 12 KB that rows off 16 bytes have as static shared memory (with 105 only one
+// block fitted and the other half of the grid waited for it).
+constexpr size_t kSmUsable = 228 * 1024, kReserved = 1024;  // of an SM; per block
+constexpr size_t room_of_two(bool full) { return (full ? 105 : 101) * 1024; }
+static_assert(2 * (room_of_two(true) + fn::norm_static(true, 512) + kReserved) <= kSmUsable &&
+                  2 * (room_of_two(false) + fn::norm_static(false, 512) + kReserved) <= kSmUsable,
+              "two blocks fit an SM");
 int stages_of(size_t room, size_t params, size_t stage) {
   if (stage == 0) return 0;
   return static_cast<int>(std::min<size_t>(fn::kMaxStages, std::max<size_t>(1, (room - params) / stage)));
@@ -280,8 +288,8 @@ extern "C" framefb_status framefb_layernorm_forward(const framefb_norm* n, frame
                        : !full && !s.wide() ? static_cast<size_t>(a.stage_bytes) * (res ? 2 : 1) * s.groups
                                             : 0;
   // two blocks on an SM where their parameters and two rows of the ring fit
-  const int per_sm = !s.wide() && params + 2 * stage <= kSmemPerSm / 2 ? 2 : 1;
-  a.stages = stages_of(kSmemPerSm / per_sm, params, stage);
+  const int per_sm = !s.wide() && params + 2 * stage <= room_of_two(full) ? 2 : 1;
+  a.stages = stages_of(per_sm == 2 ? room_of_two(full) : kSmemPerSm, params, stage);
   const int64_t blocks = std::min<int64_t>((n->N + s.groups - 1) / s.groups, static_cast<int64_t>(sms) * per_sm);
   return launch(f, grid(blocks), s.threads * s.groups, params + a.stages * stage, &a, false, stream);
 }

@@ -491,6 +491,9 @@ __device__ __forceinline__ uint32_t phase_of(const void* base, int64_t row, int6
 
 constexpr int kMaxStages = 4;
 
+// Static shared memory of norm_kernel: the sums' exchange and the masks passed on.
+constexpr size_t norm_static(bool full, int maxt) { return kMaxGroups * 2 * 32 * 4 + (full ? 1 : maxt / 32) * 512; }
+
 // Forward.  DROP, RES: whether the call drops and adds (FULL; otherwise both are looked up).
 template <typename T, bool FULL, bool DROP, bool RES, int NV, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) norm_kernel(const NormArgs a) {
@@ -502,6 +505,7 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_kernel(const NormArgs a) {
   extern __shared__ float4 dyn[];          // gamma, beta, ring
   __shared__ float sh[kMaxGroups][2][32];
   __shared__ uint4 mix[FULL ? 1 : MAXT / 32][32];
+  static_assert(sizeof(sh) + sizeof(mix) == norm_static(FULL, MAXT), "what the launch shapes count with");
   const Place p(a.groups);
   const int nvec = NV * p.T;
   int col[NV], cnt[NV];
