@@ -659,11 +659,22 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_kernel(const NormArgs a) {
 // row, has no registers left for them: norm_colsum_kernel reads dY and Z
 // too, before this kernel, which may write over them.)  Every order is fixed, so dgamma and dbeta do not depend on
 // timing.
+// xh = (Z - mean) rstd on rows far from zero: Z rstd - mean rstd in one fused
+// step has the rounding of mean * rstd in it (2e-4 of xh at a mean of 4096
+// deviations).  So either the mean goes first, as in the forward pass, one
+// instruction more; or (CARRY) that product's rounding error lo, which is
+// exact by a second fused step and the same for the whole row, is added to the
+// row's sums and to dgamma's terms.  CARRY where the first form costs more:
+// with dropout, whose 24-column variant then spills (12608 x 768 bf16 with dZin
+// 25.9 us instead of 29.8), and wide rows off 16 bytes (3600 x 9001 fp32 289
+// us instead of 322); aligned wide rows the other way (2048 x 14336 bf16 74.7
+// us, 78.8 with CARRY).
 template <typename T, bool FULL, bool DROP, int NV, int MAXT, bool WIDE>
 __global__ void __launch_bounds__(MAXT, 1) norm_grad_kernel(const NormGradArgs a) {
   using D = Deal<T, FULL>;
   constexpr int E = D::E, Q = E / 4, P2 = E / 2;
   constexpr int NA = WIDE ? 1 : NV;  // vectors whose sums are in registers (WIDE: none)
+  constexpr bool CARRY = FULL ? DROP && !WIDE : WIDE;
   constexpr bool RING = FULL && !(WIDE && sizeof(T) == 4);  // wide fp32: gamma and a row of the ring are too much
   // gamma (NV > 1); then the ring, and after it in the same place the groups' sums [2][groups][d]
   extern __shared__ float4 dyn[];
@@ -763,7 +774,7 @@ __global__ void __launch_bounds__(MAXT, 1) norm_grad_kernel(const NormGradArgs a
       if constexpr (STAGED) return st.get(arr, col[i], cnt[i]);
       return in.get(arr, i);
     };
-    const float rstd = rs1, mu = mu1;
+    const float rstd = rs1, mu = mu1, shift = -mu1 * rs1, lo = CARRY ? fmaf(-mu1, rs1, -shift) : 0.f;
     if (row + step < a.N) {
       mu1 = __ldg(a.mean + row + step);
       rs1 = __ldg(a.rstd + row + step);
@@ -778,24 +789,23 @@ __global__ void __launch_bounds__(MAXT, 1) norm_grad_kernel(const NormGradArgs a
       if constexpr (NV > 1) read_param<T, FULL>(dyn, nvec, p.tid + i * p.T, g);
 #pragma unroll
       for (int e = 0; e < P2; ++e) {
-        // the mean goes first, as in the forward pass: that difference is all but exact, while mean * rstd rounds at
-        // its own size (rows 4096 deviations from zero: 2e-4 of xh).  past the row's end dy = 0: xh there adds to no
-        // sum and is not stored
-        xh[i][e] = mul2(add2(xh[i][e], both(-mu)), both(rstd));
+        // past the row's end dy = 0: xh there adds to no sum and is not stored
+        xh[i][e] = CARRY ? fma2(xh[i][e], both(rstd), both(shift)) : mul2(add2(xh[i][e], both(-mu)), both(rstd));
         ag[i][e] = mul2(dy[e], NV > 1 ? g[e] : g1[e]);
         s1 = add2(s1, ag[i][e]);
         s2 = fma2(ag[i][e], xh[i][e], s2);
         if constexpr (!WIDE) {
           db[i][e] = add2(db[i][e], dy[e]);
-          dg[i][e] = fma2(dy[e], xh[i][e], dg[i][e]);
+          dg[i][e] = fma2(dy[e], CARRY ? add2(xh[i][e], both(lo)) : xh[i][e], dg[i][e]);
         }
       }
     }
     float s[2] = {s1.x + s1.y, s2.x + s2.y};
     group_sum(s, sh[p.group][buf], p);
     buf ^= 1;
-    // dz = rstd (a - c1 - xh c2)
-    const float c1 = s[0] * a.inv_d * rstd, c2 = s[1] * a.inv_d * rstd;
+    // dz = rstd (a - mean(a)) - xh c2, with c2 = rstd mean(a xh); xh + lo in place of xh where it is carried
+    const float c2 = (CARRY ? fmaf(lo, s[0], s[1]) : s[1]) * a.inv_d * rstd;
+    const float c1 = CARRY ? fmaf(lo, c2, s[0] * a.inv_d * rstd) : s[0] * a.inv_d * rstd;
     T* dzr = static_cast<T*>(a.dZ) + row * a.lddz;
     T* dxr = static_cast<T*>(a.dX) + row * a.lddx;
 #pragma unroll
@@ -853,12 +863,15 @@ __global__ void __launch_bounds__(MAXT, 1) norm_grad_kernel(const NormGradArgs a
 
 // Column sums of wide rows: a warp takes 32 vectors of every kSumWarps-th row
 // of the block's rows, the block joins its warps and writes one pair of rows
-// (its 32 vectors of them).  Grid: vectors of a row / 32, runs of rows.
+// (its 32 vectors of them).  Grid: vectors of a row / 32, runs of rows.  fp32
+// off 16 bytes: held to 48 registers, with which five blocks are on an SM and
+// the grid of about four takes one round (with 50, four: 3600 x 9001 gradient
+// 308 us instead of 289).
 // Bound by HBM, a second reading of dY and Z: 2048 x 14336 bf16 gradient with
 // this pass 74 us, with the sums in shared memory beside the rows 109 us.
 constexpr int kSumWarps = 8;
 template <typename T, bool FULL>
-__global__ void __launch_bounds__(32 * kSumWarps) norm_colsum_kernel(const NormGradArgs a) {
+__global__ void __launch_bounds__(32 * kSumWarps, FULL || sizeof(T) == 2 ? 0 : 5) norm_colsum_kernel(const NormGradArgs a) {
   using D = Deal<T, FULL>;
   constexpr int E = D::E, P2 = E / 2;
   __shared__ float2 sh[kSumWarps][2 * P2][32];

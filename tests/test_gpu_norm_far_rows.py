@@ -18,16 +18,18 @@ from tests.test_gpu_norm import DEV, F32, U32, assert_close, built, empty, rows,
 pytestmark = pytest.mark.gpu
 
 
-def gradients(dY, Z, gamma, mean, rstd):
+def gradients(dY, Z, gamma, mean, rstd, p=0.0):
     N, d = Z.shape
     dZ = empty(N, d, Z.dtype)
+    more = dict(dX=empty(N, d, Z.dtype), drop=ffb.framefb_dropout_params(p, 3, 4)) if p else {}
     dgamma, dbeta = (torch.full((d,), float("nan"), device=DEV) for _ in range(2))
-    ffb.framefb_layernorm_backward(dY, Z, gamma, mean, rstd, dZ, dgamma, dbeta, ws=ffb.layernorm_workspace(N, d, DEV))
+    ffb.framefb_layernorm_backward(dY, Z, gamma, mean, rstd, dZ, dgamma, dbeta, ws=ffb.layernorm_workspace(N, d, DEV), **more)
     return dZ, dgamma, dbeta
 
 
+@pytest.mark.parametrize("p", [0.0, 0.3])  # (the dropout makes dX only, by another variant of the kernel)
 @pytest.mark.parametrize("d", [768, 1023, 9000, 9001])  # in registers, unaligned; with a pass for the column sums
-def test_gradient_of_rows_far_from_zero(d):
+def test_gradient_of_rows_far_from_zero(d, p):
     rng = np.random.default_rng(d)
     N = 37
     x = rng.standard_normal((N, d))
@@ -36,7 +38,7 @@ def test_gradient_of_rows_far_from_zero(d):
     gamma = vec(1 + 0.2 * rng.standard_normal(d))
     _, mu, rs = tr.layernorm(host64(Z))
     mean, rstd = vec(mu), vec(rs)
-    dZ, dgamma, dbeta = gradients(dY, Z, gamma, mean, rstd)
+    dZ, dgamma, dbeta = gradients(dY, Z, gamma, mean, rstd, p)
     z, dy, g = host64(Z), host64(dY), host64(gamma)
     mu, rs = host64(mean)[:, None], host64(rstd)[:, None]
     dz, dg, db = tr.layernorm_grad(dy, z, g, mu[:, 0], rs[:, 0])
@@ -50,10 +52,11 @@ def test_gradient_of_rows_far_from_zero(d):
     assert_close(dbeta, db, F32, (N + 64) * U32 * np.abs(dy).sum(axis=0), "dbeta")
 
 
+@pytest.mark.parametrize("p", [0.0, 0.3])
 @pytest.mark.parametrize("d", [768, 9001])
-def test_a_constant_row_has_no_direction(d):
+def test_a_constant_row_has_no_direction(d, p):
     # xh of a row equal to its mean is 0: nothing of it reaches dgamma
     c = np.float32(1000.1)
     Z, dY = rows(np.full((3, d), c), F32), rows(np.random.default_rng(d).standard_normal((3, d)), F32)
-    _, dgamma, _ = gradients(dY, Z, None, vec([c] * 3), vec([1e-5 ** -0.5] * 3))
+    _, dgamma, _ = gradients(dY, Z, None, vec([c] * 3), vec([1e-5 ** -0.5] * 3), p)
     assert not dgamma.any()
