@@ -7,7 +7,8 @@
 //                      dZ = rstd (a - mean(a) - xh mean(a xh)) [+ dZin];  dX = drop(dZ)
 //                      dgamma = sum_t dY xh,  dbeta = sum_t dY
 //
-// All three read every input once and write every output once.
+// All three read every input once and write every output once, but for the
+// column sums of wide rows, which are a second reading of dY and Z.
 // Included by framefb_norm.cu only.
 #pragma once
 #include <cuda_bf16.h>
@@ -127,9 +128,11 @@ __device__ __forceinline__ void drop_vec(float2 (&x)[P], const DropK& k, uint32_
 // Dropout: one vector of a row per thread and step, kDropUnroll of them in
 // flight (four, with fewer warps on an SM: 35 us instead of 32 below).  Bound
 // by HBM, 2 (3 with R) passes over the array, where an element has 4 bytes:
-// 8192 x 4096 fp32 with R 57 us, 7.0 TB/s.  bf16 is bound by the generator, 20
-// wide multiplications and 20 xors per 4 columns, which keep the integer
-// multipliers 65 % and the ALUs 55 % busy: 8192 x 4096 32 us, 4.2 TB/s.
+// 8192 x 4096 fp32 with R 57 us, 7.0 TB/s.  bf16 has half the bytes to the same
+// instructions: of some 187 per 8 columns the generator's rounds are 80 (20 wide
+// multiplications and 20 xors per 4 columns), addresses, selections, scaling
+// and packing the rest.  No pipe is full (integer multipliers 65 % busy, ALUs
+// 52 %, 2.6 instructions a cycle): 8192 x 4096 32 us, 4.2 TB/s.
 // ---------------------------------------------------------------------------
 constexpr int kDropThreads = 256;
 constexpr int kDropUnroll = 2;
@@ -190,8 +193,8 @@ __global__ void __launch_bounds__(kDropThreads, 6) dropout_kernel(const DropArgs
 // Layer norm.  A block is `groups` groups of T = blockDim.x / groups threads
 // (whole warps); a group takes one row at a time and its threads hold vectors
 // t, t + T, ... (NV of them) of the row in registers, so a row is read once
-// and its mean and the sum of squared deviations from that mean (two passes
-// over registers: no cancellation) are exact fp32 sums.  Groups wait for
+// and its mean and the sum of squared deviations from that mean are fp32 sums
+// over registers, one after the other (no cancellation).  Groups wait for
 // nobody else (a named barrier each).  The rows a group takes next are on
 // their way while it works on one: without that, loads, reductions and stores
 // take turns (16384 x 4096 bf16 gradient: 245 us instead of 90).  Whole vectors come
@@ -612,7 +615,7 @@ __global__ void __launch_bounds__(MAXT, MINB) norm_kernel(const NormArgs a) {
       in.advance();
     float s[1] = {s2.x + s2.y};
     group_sum(s, sh[p.group][0], p);
-    const float mean = s[0] / static_cast<float>(a.d);  // a division: the mean of a constant row is that constant
+    const float mean = s[0] / static_cast<float>(a.d);  // a division: a constant row whose sum is exact has that constant as its mean
     if (a.Z) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) store_vec<T, FULL>(zr, col[i], cnt[i], z[i]);
